@@ -521,7 +521,12 @@ __global__ void __launch_bounds__(THREADS, kResident<MODE> / THREADS) distill_ke
                 st.inv_q = down * inv_q;
                 p_others = all.s * far * st.inv_p;
                 q_others = u_rest * inv_q;
-                st.others = all.s > 0.0f ? far * st.inv_p - u_rest * inv_q / all.s : 0.0f;
+                // p_r - q_r = p_r q_s - q_r p_s, s: all that is sent.  (Subtracted directly, two numbers next to 1 that are nearly equal leave few
+                // digits, and what is lost is common to all of the row's gradient: a factor off by 1e-3 of itself where q_r / p_r is 1 - 6e-5.)
+                Two left = Two{all.s, 0.0f}.times({all.u, 0.0f}).times({far, 0.0f}).times({down, 0.0f});
+                const Two less = Two{all.p, 0.0f}.times({near, 0.0f}).times({u_rest, 0.0f});
+                left.add(-less.hi);
+                st.others = all.s > 0.0f ? (left.hi + (left.lo - less.lo)) * st.inv_p * inv_q / all.s : 0.0f;
             }
             if (lane == 0) {
                 sh.stat = st;

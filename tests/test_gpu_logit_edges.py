@@ -1,0 +1,57 @@
+"""The logit operators where digits, forms and places are easily lost: against 64 bits, with bounds that count roundings.
+
+u = 2^-24 is one rounding of fp32, 4 u an exponential, sum_tolerance(V) the relative error of a row's sum (its derivation stands beside it).
+"""
+import math
+
+import pytest
+import torch
+
+from test_gpu_logits import B, DTYPES, INF, U, bits, check_distill, check_top, ctx, distill_reference, message, rows_of, sum_tolerance  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def messages_of(B, msg, rows):
+    return B.LogitBuffers.of(msg.idx[rows].contiguous(), msg.val[rows].contiguous(), msg.count[rows].contiguous(), msg.rest[rows].contiguous())
+
+
+# ------------------------------------------------------------------------------------------ digits of the gradient
+@pytest.mark.parametrize("T", [1.0, 2.0, 30.0])
+@pytest.mark.parametrize("N, V, k", [(40, 700, 8), (300, 5000, 8), (9, 50_257, 20), (310, 33_000, 6), (600, 66_001, 8)])
+def test_gradient_outside_the_message_keeps_its_digits(B, ctx, N, V, k, T):
+    """Flat rows of a student next to its teacher: of an unsent logit's gradient w T p_i (1 - q_r / p_r) all but 1e-5 or so cancels.
+
+    1 - q_r / p_r = (p_r q_s - q_r p_s) / p_r, with p_s and q_s what is sent, so the difference is off by the errors of both products, each of
+    at most three sums and exponentials: relative errors of terms as small as p_s.  What it is multiplied by is as exact as everywhere."""
+    z = rows_of(V, N, torch.float32, V, scale=0.3)
+    t = z.double()
+    idx = torch.rand((N, V), generator=torch.Generator(device="cuda").manual_seed(3), device="cuda").topk(k, 1).indices
+    val = (t.gather(1, idx) + 0.02 * T * torch.randn((N, k), generator=torch.Generator(device="cuda").manual_seed(4), device="cuda")).float()
+    behind = t.scatter(1, idx, -INF)
+    rest = torch.logsumexp((behind - val.double().max(1, keepdim=True).values) / T, 1).float()
+    msg = B.LogitBuffers.of(idx.int().contiguous(), val.contiguous(), torch.full((N,), k, dtype=torch.int32, device="cuda"), rest)
+    weight = torch.rand(N, device="cuda") + 0.5
+    sent = torch.zeros((N, V), dtype=torch.bool, device="cuda").scatter_(1, idx, True)
+    x = t / T
+    ln_p = x - torch.logsumexp(x, 1, keepdim=True)
+    p_s = ln_p.gather(1, idx).exp().sum(1, keepdim=True)
+    p_r = torch.logsumexp(torch.where(sent, -INF, ln_p), 1, keepdim=True).exp()
+    parts = torch.cat([val.double() / T, val.double().max(1, keepdim=True).values / T + rest.double()[:, None]], 1)
+    q = torch.softmax(parts, 1)
+    q_r, q_s = q[:, -1:], q[:, :-1].sum(1, keepdim=True)
+    left = p_r * q_s - q_r * p_s
+    scale = weight.double()[:, None] * T * ln_p.exp() / p_r
+    want = scale * left
+    assert float((left.abs() / p_r).median()) < 1e-3
+    span = float((x.max(1).values - x.min(1).values).max())
+    eps = sum_tolerance(V) + (8 + 3 * span) * U
+    off = scale * (3 * eps * (p_r * q_s + q_r * p_s) + left.abs() * (3 * eps + (16 + 3 * span) * U)) + want.abs() * U + 1e-37
+    for apart in (False, True):
+        buf, grad = B.DistillBuffers(N), torch.full_like(z, 7.0)
+        B.mlmc_distill(ctx, z, msg, T, True, weight, buf, None if apart else grad)
+        if apart:
+            B.mlmc_distill_grad(ctx, z, msg, T, True, weight, buf, grad)
+        err = (grad.double() - want).abs()
+        assert (err <= off)[~sent].all(), (apart, float((err / off)[~sent].max()))
+    assert B.mlmc_get_status(ctx) == B.MLMC_OK
