@@ -507,11 +507,10 @@ __global__ void __launch_bounds__(THREADS, kResident<MODE> / THREADS) distill_ke
                 st.m_r = st.others = st.m = st.inv_p = st.t_max = st.inv_q = CUDART_NAN_F;
             } else {
                 // p is next to exp(m / T), q next to exp(t_max / T) times e^up
-                constexpr float kLog2e = 1.44269504f;
                 const float far = exp2_approx((all.m - m) * c), near = exp2_approx((z_max - m) * c);
                 up = fmaxf(rest, 0.0f);
-                down = exp2_approx(-up * kLog2e);
-                const float u_rest = exp2_approx((rest - up) * kLog2e);
+                down = exp_of(-up);
+                const float u_rest = exp_of(rest - up);
                 p_all = all.p * near + all.s * far;
                 st.m_r = all.m;
                 st.m = m;

@@ -367,6 +367,14 @@ __device__ __forceinline__ Two log_of(float s) {
     return ln;
 }
 
+// exp(x), x <= 0, of which -inf is one: x log2(e) is rounded nowhere (as one number it would be off by 2^-20 at x = -14, and so would
+// everything that is multiplied by the result).
+__device__ __forceinline__ float exp_of(float x) {
+    constexpr float kLog2e = 1.44269502f, kLog2eLow = 1.92596299e-8f;
+    const float y = x * kLog2e, r = exp2_approx(y), low = fmaf(x, kLog2e, -y) + x * kLog2eLow;
+    return r > 0.0f ? fmaf(r * low, 0.693147181f, r) : 0.0f;
+}
+
 // Numbers ordered like the logits: larger for larger ones, the same for -0 and 0.
 __device__ __forceinline__ uint32_t logit_key(float v) {
     const uint32_t u = __float_as_uint(v + 0.0f);

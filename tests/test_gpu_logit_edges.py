@@ -55,3 +55,25 @@ def test_gradient_outside_the_message_keeps_its_digits(B, ctx, N, V, k, T):
         err = (grad.double() - want).abs()
         assert (err <= off)[~sent].all(), (apart, float((err / off)[~sent].max()))
     assert B.mlmc_get_status(ctx) == B.MLMC_OK
+
+
+def test_teacher_probabilities_next_to_a_large_rest(B, ctx):
+    """Two buckets, a message of one entry and the rest: q = 1 / (1 + e^rest) and what is left of 1.  An exponential, the sum, the division and
+    two products: 8 u.  The student says nothing of what is read off here, so the gradient is -q."""
+    rest = torch.cat([torch.linspace(0.01, 80.0, 3000), torch.linspace(-80.0, -0.01, 3000), torch.tensor([-INF, 0.0, 84.0])]).cuda()
+    N, V = rest.numel(), 9
+    zero = torch.zeros((N, 1), device="cuda")
+    msg = B.LogitBuffers.of(zero.int(), zero + 2.5, torch.ones(N, dtype=torch.int32, device="cuda"), rest)
+    for others in (True, False):
+        z = torch.zeros((N, V), device="cuda")
+        if others:
+            z[:, 0] = -INF
+            want, at = torch.sigmoid(-rest.double()), 0
+        else:
+            z[:, 1], z[:, 2:] = -300.0, -INF
+            want, at = torch.sigmoid(rest.double()), 1
+        grad = torch.full_like(z, 7.0)
+        B.mlmc_distill(ctx, z, msg, 1.0, True, None, B.DistillBuffers(N), grad)
+        err = (-grad[:, at].double() - want).abs()
+        assert (err <= 8 * U * want + 1e-37).all(), (others, float((err / want / U)[want > 0].max()))
+    assert B.mlmc_get_status(ctx) == B.MLMC_OK
