@@ -263,14 +263,14 @@ int mlmc_top_logits(mlmc_ctx* ctx, const void* logits, int dtype, int64_t V, int
  *         (MLMC_ERR_NONFINITE), an index >= V or twice in the message, count outside 0..k (MLMC_ERR_ARG); its gradient is NaN too.
  *   stat  [N][8] fp32, what mlmc_distill_grad needs; or NULL.
  *   grad  NULL, or dtype [N][ldg]: weight_n dloss_n/dz in the same call.  It may be the logits themselves
- *         (same address, ldg = ld).
+ *         (same address, ldg = ld), and with ldg = ld its rows may lie between theirs (the other columns of one buffer).
  *   weight device fp32 [N] or NULL (1): the rows' weights in what is differentiated; not used where grad is NULL. */
 int mlmc_distill(mlmc_ctx* ctx, const void* logits, int dtype, int64_t V, int64_t N, int64_t ld, const mlmc_logit_msgs* msgs, double T,
                  int rest, const float* weight, float* loss, float* stat, void* grad, int64_t ldg, void* stream);
 
 /* The gradient by itself, of the logits, messages, T and rest that mlmc_distill made `stat` from:
  *     dz_i = weight T (p_i - q_i) for i in the message; weight T p_i (1 - q_rest / p_rest), with rest = 0 weight T p_i, for the others.
- * grad may be the logits themselves (same address, ldg = ld). */
+ * grad as above. */
 int mlmc_distill_grad(mlmc_ctx* ctx, const void* logits, int dtype, int64_t V, int64_t N, int64_t ld, const mlmc_logit_msgs* msgs,
                       double T, int rest, const float* weight, const float* stat, void* grad, int64_t ldg, void* stream);
 

@@ -126,7 +126,8 @@ int check_messages(const mlmc_logit_msgs* m, int64_t N, bool rest) {
     return m->k >= 1 && m->k <= MLMC_MAX_TOP_LOGITS ? MLMC_OK : MLMC_ERR_ARG;
 }
 
-// The gradient's rows: the logits' own, or memory that does not overlap them.
+// The gradient's rows: the logits' own, or memory apart from them; between them too (the other columns of one buffer) where both have one
+// stride, so that what holds for a row holds for all.
 int check_gradient(const void* logits, int dtype, int64_t V, int64_t N, int64_t ld, const void* grad, int64_t ldg) {
     const int64_t size = dtype == MLMC_BF16 ? 2 : 4;
     if (ldg < V || ldg > INT64_MAX / 8 / kMostRows || reinterpret_cast<uintptr_t>(grad) % size != 0) return MLMC_ERR_ARG;
@@ -134,7 +135,11 @@ int check_gradient(const void* logits, int dtype, int64_t V, int64_t N, int64_t 
     if (grad == logits) return ld == ldg || N == 1 ? MLMC_OK : MLMC_ERR_ARG;
     const uintptr_t a = reinterpret_cast<uintptr_t>(logits), b = reinterpret_cast<uintptr_t>(grad);
     const uintptr_t a_end = a + (uintptr_t)(((N - 1) * ld + V) * size), b_end = b + (uintptr_t)(((N - 1) * ldg + V) * size);
-    return a_end <= b || b_end <= a ? MLMC_OK : MLMC_ERR_ARG;
+    if (a_end <= b || b_end <= a) return MLMC_OK;
+    if (ld != ldg) return MLMC_ERR_ARG;
+    const uintptr_t row = (uintptr_t)(V * size), stride = (uintptr_t)(ld * size);
+    const uintptr_t apart = b > a ? (b - a) % stride : (stride - (a - b) % stride) % stride;  // from a row of logits to the gradient's next
+    return apart >= row && apart + row <= stride ? MLMC_OK : MLMC_ERR_ARG;
 }
 
 // Beams of one state lie apart, and so do source and destination unless they are the same.

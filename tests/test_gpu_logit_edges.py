@@ -77,3 +77,26 @@ def test_teacher_probabilities_next_to_a_large_rest(B, ctx):
         err = (-grad[:, at].double() - want).abs()
         assert (err <= 8 * U * want + 1e-37).all(), (others, float((err / want / U)[want > 0].max()))
     assert B.mlmc_get_status(ctx) == B.MLMC_OK
+
+
+# ------------------------------------------------------------------------------------------ where the gradient may lie
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N, V, gap", [(1, 300, 0), (7, 300, 0), (7, 301, 3), (40, 50_257, 1), (600, 9000, 0), (600, 66_001, 1)])
+def test_gradient_in_the_other_columns_of_one_buffer(B, ctx, N, V, gap, dtype):
+    memory = torch.full((N, 2 * V + gap), 7.0, dtype=dtype, device="cuda")
+    for left in (True, False):
+        z, grad = (memory[:, :V], memory[:, V + gap:]) if left else (memory[:, V + gap:], memory[:, :V])
+        z.copy_(rows_of(V, N, dtype, V))
+        kept = z.clone()
+        msg = message(B, rows_of(V, N, torch.float32, V + 1), 12, 1.0)
+        want, loss = torch.zeros((N, V), dtype=dtype, device="cuda"), B.DistillBuffers(N)
+        B.mlmc_distill(ctx, z, msg, 1.0, True, None, loss, want)
+        buf = B.DistillBuffers(N)
+        B.mlmc_distill(ctx, z, msg, 1.0, True, None, buf, grad)
+        assert torch.equal(grad, want) and torch.equal(buf.loss, loss.loss) and torch.equal(bits(z.contiguous()), bits(kept))
+        grad.fill_(5.0)
+        B.mlmc_distill_grad(ctx, z, msg, 1.0, True, None, buf, grad)
+        B.mlmc_distill_grad(ctx, z, msg, 1.0, True, None, buf, want)
+        assert torch.equal(grad, want) and torch.equal(bits(z.contiguous()), bits(kept))
+        assert (memory[:, V:V + gap] == 7.0).all()
+    assert B.mlmc_get_status(ctx) == B.MLMC_OK
