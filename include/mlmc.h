@@ -284,8 +284,11 @@ typedef struct {
 
 /* One step of beam search: of the W V continuations of every sentence the K best.  W <= MLMC_MAX_BEAMS, K <= MLMC_MAX_BEAMS_OUT.
  *   rows   the messages of the logits of the B W beams (sentence b, beam w in row b W + w), made by mlmc_top_logits with this T and
- *          k >= min(K, V).  Continuation j of beam w has the score  score_w + ln softmax(z_w / T)_j,  compared in fp64; equal
- *          scores, those of beams with the same score and message among them, go to the lower beam, then to the order of its row.
+ *          k >= min(K, V).  Continuation j of beam w has the score  score_w + ln softmax(z_w / T)_j.  A beam's own continuations keep the
+ *          order of its row.  Between beams the logarithm is as exact as `rest`, an fp32 number (off by up to 6e-7 in rows of 2000 to
+ *          131,072 logits): continuations of two beams that are nearer than both rows' errors may come in either order.  Equal scores,
+ *          those of beams with the same score and message (and rests that agree to 2^-20) among them, go to the lower beam, then to the
+ *          order of its row.
  *   score  [B][W] scores so far; -inf: the beam does not exist (the first step has one beam per sentence).  NaN and +inf set
  *          MLMC_ERR_NONFINITE, and the beam counts as none.
  *   done   [B][W] or NULL: a beam that has ended is its own only continuation, token eos, score unchanged; its row is not looked at.

@@ -100,3 +100,38 @@ def test_gradient_in_the_other_columns_of_one_buffer(B, ctx, N, V, gap, dtype):
         assert torch.equal(grad, want) and torch.equal(bits(z.contiguous()), bits(kept))
         assert (memory[:, V:V + gap] == 7.0).all()
     assert B.mlmc_get_status(ctx) == B.MLMC_OK
+
+
+# ------------------------------------------------------------------------------------------ beams that are nearly equal
+@pytest.mark.parametrize("T", [1.0, 2.0])
+@pytest.mark.parametrize("V, scale", [(40, 1.0), (5000, 0.5), (50_257, 3.0)])
+def test_continuations_of_two_beams_next_to_one_another(B, ctx, V, scale, T):
+    """Best continuations up to 4e-6 apart: as far as the rows' sums tell beams apart, they come in order; a beam's own always do."""
+    Bn, W, K = 300, 2, 6
+    g = torch.Generator(device="cuda").manual_seed(V)
+    z = torch.randn((Bn * W, V), generator=g, device="cuda") * scale
+    x = z.double() / T
+    ln_p = (x - torch.logsumexp(x, 1, keepdim=True)).reshape(Bn, W, V)
+    top = ln_p.max(2).values
+    score = -5.0 - torch.rand((Bn, W), generator=g, device="cuda")
+    apart = (torch.rand(Bn, generator=g, device="cuda").double() - 0.5) * 8e-6
+    score[:, 1] = (score[:, 0].double() + top[:, 0] - top[:, 1] + apart).float()
+    rows, out = B.LogitBuffers(Bn * W, K), B.BeamBuffers(Bn, K)
+    B.mlmc_top_logits(ctx, z, None, T, rows)
+    B.mlmc_beam_select(ctx, rows, V, W, T, score, None, -1, out)
+    total = score.double()[:, :, None] + ln_p
+    best, at = torch.sort(total.reshape(Bn, -1), dim=1, descending=True, stable=True)
+    tol = sum_tolerance(V, K) + U * math.log(V)                  # of a row's logarithm, as in the tests of the selection
+    flat = out.parent.long() * V + out.token.long()
+    mine = total.reshape(Bn, -1).gather(1, flat)
+    assert ((out.score.double() - mine).abs() <= tol + U * mine.abs()).all()
+    assert (out.score[:, 1:] <= out.score[:, :-1]).all()
+    assert ((mine - best[:, :K]).abs() <= 2 * tol).all()
+    clear = (best[:, :K] - best[:, 1:K + 1] > 2 * tol).all(1)
+    assert torch.equal(flat[clear], at[:, :K][clear])
+    order = torch.sort(z.double(), dim=1, descending=True, stable=True).indices.reshape(Bn, W, V)
+    for w in range(W):                                           # the beam's tokens are the first ones of its row, in order
+        place = (out.parent == w).long().cumsum(1) - 1
+        want = order[:, w].gather(1, place.clamp(min=0))
+        assert torch.equal(out.token.long()[out.parent == w], want[out.parent == w])
+    assert B.mlmc_get_status(ctx) == B.MLMC_OK
