@@ -230,7 +230,7 @@ int mlmc_aggregate_topk_noalloc(const mlmc_topk_msgs* msgs, int M, int64_t d, fl
  * Conventions, beside those above
  *  - Logits are [N][ld] fp32 or bf16, row stride ld >= V elements, V <= 2^20, N <= 2^24.  Rows may start at any element; rows on
  *    16-byte boundaries are read fastest.  None of the limits d_max, M_max, L_max of the context applies.
- *  - Order of a row: larger logits first, equal ones (-0 and 0 are equal) by ascending index.
+ *  - Order of a row: larger logits first, equal ones (-0 and 0 are equal; a message has 0 for both) by ascending index.
  *  - -inf is a logit of probability 0 and enters no message; NaN and +inf make the row void and set MLMC_ERR_NONFINITE.
  *  - T is the temperature, 1e-3 <= T <= 1e3; it divides the logits.
  *  - Buffers of a call do not overlap unless that is said. */
@@ -243,7 +243,7 @@ int mlmc_aggregate_topk_noalloc(const mlmc_topk_msgs* msgs, int M, int64_t d, fl
 typedef struct {
     uint32_t* idx;     /* [N][k] indices, in the order of the row                                               */
     float*    val;     /* [N][k] their logits                                                                   */
-    int32_t*  count;   /* [N] entries used; the rest of the row's k places is neither written nor read          */
+    int32_t*  count;   /* [N] entries used; the rest of the row's k places is not written, and has no influence */
     float*    rest;    /* [N] ln sum exp((z_j - max val) / T) over all j outside the message, -inf: none there  */
     int32_t   k;       /* 1 <= k <= MLMC_MAX_TOP_LOGITS                                                         */
 } mlmc_logit_msgs;

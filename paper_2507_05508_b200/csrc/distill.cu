@@ -279,6 +279,7 @@ __global__ void __launch_bounds__(THREADS, kResident<MODE> / THREADS) distill_ke
     int n;
     uint32_t j;
     float val, z;
+    // (Places behind the message are read too and not used: waiting for the count first costs 0.15 us a call, rows that are held 2 %.)
     auto ask_message = [&](int64_t at) {
         n = at < p.N ? p.count[at] : 0;
         const bool mine = at < p.N && t < p.k;
