@@ -178,6 +178,7 @@ def _host_array(ctype, values: Optional[Sequence]):
 def mlmc_create(device: int, d_max: int, M_max: int, L_max: int) -> C.c_void_p:
     ctx = C.c_void_p()
     _check(lib().mlmc_create(C.byref(ctx), device, d_max, M_max, L_max), "mlmc_create")
+    ctx.device = device
     return ctx
 
 
@@ -351,7 +352,10 @@ def _vector(x: Optional[torch.Tensor], dtype, numel: int, device, what: str):
     return x.data_ptr()
 
 
-def _stream_of(device) -> int:
+def _stream_of(ctx, device) -> int:
+    """The current stream of the tensors' GPU, which has to be the context's: a kernel on another one cannot reach them."""
+    if getattr(ctx, "device", device.index) != device.index:
+        raise ValueError(f"the tensors are on {device}, the context is of GPU {ctx.device}")
     return torch.cuda.current_stream(device).cuda_stream if _raw_stream is None else _raw_stream(device.index)
 
 
@@ -366,7 +370,7 @@ def mlmc_top_logits(ctx, logits: torch.Tensor, skip: Optional[torch.Tensor], T: 
     ptr, dt, v, n, ld = _rows(logits)
     dev = logits.device
     _check(lib().mlmc_top_logits(ctx, ptr, dt, v, n, ld, _vector(skip, torch.uint8, n, dev, "skip"), T, _messages(out, n, dev),
-                                 _stream_of(dev)), "mlmc_top_logits")
+                                 _stream_of(ctx, dev)), "mlmc_top_logits")
 
 
 def _grad_rows(logits: torch.Tensor, grad: torch.Tensor):
@@ -390,7 +394,7 @@ def mlmc_distill(ctx, logits: torch.Tensor, msgs: "LogitBuffers", T: float, rest
     gp, ldg = (None, v) if grad is None else _grad_rows(logits, grad)
     _check(lib().mlmc_distill(ctx, ptr, dt, v, n, ld, _messages(msgs, n, dev), T, 1 if rest else 0,
                               _vector(weight, torch.float32, n, dev, "weight"), out.loss_ptr, out.stat_ptr, gp, ldg,
-                              _stream_of(dev)), "mlmc_distill")
+                              _stream_of(ctx, dev)), "mlmc_distill")
 
 
 def mlmc_distill_grad(ctx, logits: torch.Tensor, msgs: "LogitBuffers", T: float, rest: bool, weight: Optional[torch.Tensor],
@@ -401,7 +405,7 @@ def mlmc_distill_grad(ctx, logits: torch.Tensor, msgs: "LogitBuffers", T: float,
     _loss_buffers(out, n, dev)
     gp, ldg = _grad_rows(logits, grad)
     _check(lib().mlmc_distill_grad(ctx, ptr, dt, v, n, ld, _messages(msgs, n, dev), T, 1 if rest else 0,
-                                   _vector(weight, torch.float32, n, dev, "weight"), out.stat_ptr, gp, ldg, _stream_of(dev)),
+                                   _vector(weight, torch.float32, n, dev, "weight"), out.stat_ptr, gp, ldg, _stream_of(ctx, dev)),
            "mlmc_distill_grad")
 
 
@@ -413,7 +417,7 @@ def mlmc_beam_select(ctx, rows: "LogitBuffers", V: int, W: int, T: float, score:
         raise ValueError("the beams are on another device than the messages")
     _check(lib().mlmc_beam_select(ctx, _messages(rows, n, dev), V, out.B, W, T, _vector(score, torch.float32, n, dev, "score"),
                                   _vector(done, torch.uint8, n, dev, "done"), eos, out.K,
-                                  out.ref if done is not None else out.ref_endless, _stream_of(dev)), "mlmc_beam_select")
+                                  out.ref if done is not None else out.ref_endless, _stream_of(ctx, dev)), "mlmc_beam_select")
 
 
 def mlmc_beam_reorder(ctx, parent: torch.Tensor, states: "BeamStates") -> None:
@@ -421,7 +425,7 @@ def mlmc_beam_reorder(ctx, parent: torch.Tensor, states: "BeamStates") -> None:
     if parent.device != states.device or parent.numel() != states.beams or parent.dtype != torch.int32 or not parent.is_contiguous():
         raise ValueError(f"parent is a contiguous int32 tensor of {states.beams} elements on {states.device}")
     _check(lib().mlmc_beam_reorder(ctx, parent.data_ptr(), states.beams // states.W, states.W, states.array, states.n,
-                                   _stream_of(states.device)), "mlmc_beam_reorder")
+                                   _stream_of(ctx, states.device)), "mlmc_beam_reorder")
 
 
 class LogitBuffers:

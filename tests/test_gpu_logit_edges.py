@@ -2,6 +2,7 @@
 
 u = 2^-24 is one rounding of fp32, 4 u an exponential, sum_tolerance(V) the relative error of a row's sum (its derivation stands beside it).
 """
+import ctypes as C
 import math
 
 import pytest
@@ -135,3 +136,17 @@ def test_continuations_of_two_beams_next_to_one_another(B, ctx, V, scale, T):
         want = order[:, w].gather(1, place.clamp(min=0))
         assert torch.equal(out.token.long()[out.parent == w], want[out.parent == w])
     assert B.mlmc_get_status(ctx) == B.MLMC_OK
+
+
+# ------------------------------------------------------------------------------------------ refusals
+def test_tensors_on_another_gpu_than_the_context(B, ctx):
+    assert ctx.device == 0
+    other = C.c_void_p(ctx.value)
+    other.device = 1
+    z, rows, buf, out = torch.zeros((4, 10), device="cuda"), B.LogitBuffers(4, 3), B.DistillBuffers(4), B.BeamBuffers(2, 2)
+    for call in (lambda: B.mlmc_top_logits(other, z, None, 1.0, rows), lambda: B.mlmc_distill(other, z, rows, 1.0, True, None, buf, None),
+                 lambda: B.mlmc_distill_grad(other, z, rows, 1.0, True, None, buf, z),
+                 lambda: B.mlmc_beam_select(other, rows, 10, 2, 1.0, z[0, :4], None, -1, out),
+                 lambda: B.mlmc_beam_reorder(other, out.parent, B.BeamStates([z], 2))):
+        with pytest.raises(ValueError, match="GPU"):
+            call()

@@ -1,4 +1,6 @@
 """What the logit operators accept and refuse beside the plain refusals, without a GPU: a call that passes its checks ends with MLMC_ERR_CUDA."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -18,3 +20,12 @@ pytestmark = pytest.mark.skipif(torch.cuda.is_available(), reason="a made-up con
 def test_gradient_rows_between_the_logits(ctx, at, ld, ldg, N, ok):
     want = B.MLMC_ERR_CUDA if ok else B.MLMC_ERR_ARG
     assert distill(ctx, N=N, ld=ld, ldg=ldg, grad=P + at) == distill_grad(ctx, N=N, ld=ld, ldg=ldg, grad=P + at) == want
+
+
+def test_tensors_on_another_gpu_than_the_context():
+    """A kernel of one GPU on another's memory would fault: the binding looks before it calls."""
+    here = C.c_void_p(P)
+    here.device = 1
+    for at in ("cuda:0", "cuda:2"):
+        with pytest.raises(ValueError):
+            B._stream_of(here, torch.device(at))
