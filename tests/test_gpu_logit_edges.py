@@ -138,6 +138,154 @@ def test_continuations_of_two_beams_next_to_one_another(B, ctx, V, scale, T):
     assert B.mlmc_get_status(ctx) == B.MLMC_OK
 
 
+# ------------------------------------------------------------------------------------------ the rest, wherever it lies
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N, V, k", [(3, 1 << 20, 1024), (3, 1 << 20, 512), (4, 262_147, 700), (40, 131_075, 128), (330, 131_075, 128),
+                                     (300, 40_000, 300), (20, 9001, 1000), (500, 3001, 60), (330, 1244, 64), (300, 398, 99)])
+def test_a_rest_of_a_few_logits(B, ctx, N, V, k, dtype):
+    """All but the message and n <= 12 logits of 0 is -inf, or so low that it does not count: one of them that is lost, or taken twice, changes
+    the rest by 1 / 12.  They lie at both ends of the row, around the borders of sections, and anywhere.  rest = ln n - max: a sum of n
+    ones, an exponential or two on the way, the rounding of the result."""
+    g = torch.Generator(device="cuda").manual_seed(V + k)
+    for low, ld, offset in ((-INF, V + 5, 3), (-200.0, V, 0)):
+        z = rows_of(V, N, dtype, 1, ld=ld, offset=offset)
+        z.fill_(low)
+        place = torch.rand((N, V), generator=g, device="cuda")
+        border = torch.tensor([b * V // n + d for n in (2, 4, 8) for b in range(1, n) for d in (-9, -1, 0, 1, 8)], device="cuda").clamp(0, V - 1)
+        few = torch.cat([torch.tensor([0, 1, V - 2, V - 1], device="cuda").expand(N, 4),
+                         border[torch.randint(0, border.numel(), (N, 4), generator=g, device="cuda")],
+                         torch.randint(0, V, (N, 4), generator=g, device="cuda")], 1)
+        place.scatter_(1, few, -1.0)                                           # the message lies anywhere else
+        sent = place.topk(k, 1).indices
+        z.scatter_(1, few, torch.zeros((N, 12), dtype=dtype, device="cuda"))
+        z.scatter_(1, sent, (20.0 + 4.0 * torch.rand((N, k), generator=g, device="cuda")).to(dtype))
+        n = (z == 0).sum(1)
+        out = B.LogitBuffers(N, k)
+        B.mlmc_top_logits(ctx, z, None, 1.0, out)
+        assert (out.count == k).all()
+        assert torch.equal(out.idx.long().sort(1).values, sent.sort(1).values)
+        want = n.double().log() - z.max(1).values.double()
+        assert ((out.rest.double() - want).abs() <= (12 + 4 * 4) * U + 2 * U * want.abs()).all()
+    assert B.mlmc_get_status(ctx) == B.MLMC_OK
+
+
+# ------------------------------------------------------------------------------------------ rows that are held in shared memory
+@pytest.mark.parametrize("rest", [True, False])
+@pytest.mark.parametrize("V, k", [(66_001, 300), (131_075, 1024), (131_075, 257)])
+def test_long_messages_of_rows_that_are_held(B, ctx, V, k, rest):
+    """fp32 rows that clusters hold between their two passes, with more entries than the cluster's blocks have threads; the next row's
+    message is asked for while this one's is in use, whatever its count says."""
+    N = 605
+    z = rows_of(V, N, torch.float32, 71, scale=2.0)
+    t = torch.randn((N, V), generator=torch.Generator(device="cuda").manual_seed(72), device="cuda") * 1.5
+    val, idx = t.topk(k, 1)
+    behind = torch.cat([a.double().scatter(1, i, -INF).logsumexp(1) for a, i in zip(t.split(100), idx.split(100))])
+    del t
+    mix = torch.rand((N, k), generator=torch.Generator(device="cuda").manual_seed(73), device="cuda").argsort(1)      # in any order
+    msg = B.LogitBuffers.of(idx.gather(1, mix).int().contiguous(), val.gather(1, mix).contiguous(),
+                            torch.full((N,), k, dtype=torch.int32, device="cuda"), (behind - val[:, 0].double()).float())
+    row = torch.arange(N, device="cuda")
+    wrong = (row % 50 == 7) | (row == 0) | (row == N - 1)
+    msg.count[wrong] = torch.where(row % 2 == 0, -1, k + 1)[wrong].int()
+    msg.count[row % 50 == 8] = 0
+    msg.count[row % 50 == 9] = 256
+    buf, grad = B.DistillBuffers(N), torch.full((N, V), 7.0, device="cuda")
+    B.mlmc_distill(ctx, z, msg, 1.0, rest, None, buf, grad)
+    assert B.mlmc_get_status(ctx) == B.MLMC_ERR_ARG
+    assert torch.isnan(buf.loss[wrong]).all() and torch.isnan(grad[wrong]).all()
+    assert not torch.isnan(buf.loss[~wrong]).any() and not torch.isnan(grad[~wrong]).any()
+    assert (buf.loss[row % 50 == 8] == 0).all() and (grad[row % 50 == 8] == 0).all()
+    some = torch.tensor([1, 6, 8, 9, 10, 300, 359, 602, 603], device="cuda")
+    loss, want, loss_off, off = distill_reference(z[some], messages_of(B, msg, some), 1.0, rest, None)
+    assert ((buf.loss[some].double().cpu() - loss).abs() <= loss_off).all()
+    assert ((grad[some].double() - want).abs() <= off + (want.abs() + off) * U + 1e-37).all()
+    kept = z.clone()
+    B.mlmc_distill(ctx, z, msg, 1.0, rest, None, buf, z)                       # over the logits
+    assert torch.equal(bits(z)[~wrong], bits(grad)[~wrong]) and torch.isnan(z[wrong]).all()
+    assert B.mlmc_get_status(ctx) == B.MLMC_ERR_ARG
+    B.mlmc_distill(ctx, kept, msg, 1.0, rest, None, buf, None)                 # the loss by itself, the gradient by itself
+    assert B.mlmc_get_status(ctx) == B.MLMC_ERR_ARG
+    B.mlmc_distill_grad(ctx, kept, msg, 1.0, rest, None, buf, grad)
+    assert torch.isnan(grad[wrong]).all()
+    assert ((grad[some].double() - want).abs() <= off + (want.abs() + off) * U + 1e-37).all()
+    assert B.mlmc_get_status(ctx) == B.MLMC_OK
+
+
+# ------------------------------------------------------------------------------------------ padding
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_two_call_gradient_of_every_row_of_a_padded_batch(B, ctx, dtype):
+    V, N = 9000, 40
+    z = rows_of(V, N, dtype, 4)
+    count = torch.arange(N, device="cuda") % 4 * 5                               # 0, 5, 10, 15 of 15 places
+    msg = message(B, rows_of(V, N, torch.float32, 5), 15, 1.0, count)
+    weight = torch.rand(N, device="cuda")
+    loss, want, loss_off, off = distill_reference(z, msg, 1.0, True, weight)
+    z[count == 0] = float("nan")
+    buf, grad = B.DistillBuffers(N), torch.full_like(z, 7.0)
+    B.mlmc_distill(ctx, z, msg, 1.0, True, weight, buf, None)
+    B.mlmc_distill_grad(ctx, z, msg, 1.0, True, weight, buf, grad)
+    assert ((buf.loss.double().cpu() - loss).abs() <= loss_off).all() and (buf.loss[count == 0] == 0).all()
+    assert ((grad.double() - want).abs() <= off + (want.abs() + off) * torch.finfo(dtype).eps / 2 + 1e-37).all() and (grad[count == 0] == 0).all()
+    assert B.mlmc_get_status(ctx) == B.MLMC_OK
+
+
+# ------------------------------------------------------------------------------------------ the temperature's range
+@pytest.mark.parametrize("rest", [True, False])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T", [1e-3, 0.05, 30.0, 1e3])
+def test_distillation_at_the_ends_of_the_temperature(B, ctx, T, dtype, rest):
+    for N, V, k in ((5, 400, 30), (3, 8193, 64), (2, 60_001, 40)):
+        z = rows_of(V, N, dtype, V, scale=2.0)
+        t = z.float() * 0.7 + rows_of(V, N, torch.float32, V + 1, scale=1.0)
+        check_distill(B, ctx, z, message(B, t, k, T), T, rest, torch.rand(N, device="cuda") + 0.1)
+    # logits as far apart as the temperature makes them look near, and as near as it makes them look far
+    z = (rows_of(3000, 4, torch.float32, 9, scale=2.0) * T).to(dtype)
+    t = z.float() + rows_of(3000, 4, torch.float32, 10, scale=0.5) * T
+    check_distill(B, ctx, z, message(B, t, 40, T), T, rest)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T", [1e-3, 0.05, 30.0, 1e3])
+def test_ends_of_the_type_at_the_ends_of_the_temperature(B, ctx, T, dtype):
+    V, lowest = 3000, torch.finfo(dtype).min
+    z = rows_of(V, 6, dtype, 9, scale=2.0)
+    t = rows_of(V, 6, torch.float32, 10, scale=2.0)
+    t[:, :60] += 20.0                       # messages of the first 60 indices
+    z[0, 100:] = lowest                     # masked with the type's lowest value
+    z[1, 100:] = -INF                       # masked with -inf: probability 0
+    z[2] = lowest                           # all equal
+    z[3, 7] = torch.finfo(dtype).max / max(2.0, 2.0 * T)   # one above everything: a loss of nearly T times that, below what fp32 has
+    z[4, 60:] -= 300.0
+    msg = message(B, t, 40, T)
+    check_distill(B, ctx, z, msg, T, True)
+    check_distill(B, ctx, z, msg, T, False)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T", [30.0, 100.0, 1e3])
+@pytest.mark.parametrize("N, V, k", [(300, 400, 30), (7, 50_257, 64), (40, 131_072, 100)])
+def test_small_losses_keep_their_digits_at_high_temperatures(B, ctx, N, V, k, T, dtype):
+    """The bound of the test at lower temperatures, which says where its terms come from."""
+    z = rows_of(V, N, dtype, 61, scale=2.0)
+    t = z.float() + 0.02 * T * rows_of(V, N, torch.float32, 62, scale=1.0)
+    msg = message(B, t, k, T)
+    buf = B.DistillBuffers(N)
+    B.mlmc_distill(ctx, z, msg, T, True, None, buf, None)
+    eps = sum_tolerance(V)
+    x = z.double() / T
+    ln_p = x - torch.logsumexp(x, 1, keepdim=True)
+    sent = torch.zeros((N, V), dtype=torch.bool, device="cuda").scatter_(1, msg.idx.long(), True)
+    ln_p = torch.cat([ln_p.gather(1, msg.idx.long()), torch.logsumexp(torch.where(sent, -INF, ln_p), 1, keepdim=True)], 1)
+    ln_q = torch.log_softmax(torch.cat([msg.val.double() / T, msg.val[:, :1].double() / T + msg.rest[:, None].double()], 1), 1)
+    q, apart = ln_q.exp(), (ln_q.exp() - ln_p.exp()).abs()
+    want = T * T * (q * (ln_q - ln_p)).sum(1)
+    spread = (ln_q.max(1).values - ln_q.min(1).values)
+    off = T * T * (2 * eps * apart[:, -1] + 2 * U * apart.sum(1)) + want * (2 * eps + (24 + 6 * spread) * U) + T * T * eps * eps
+    assert float(want.max()) < 0.05 * T * T
+    assert ((buf.loss.double() - want).abs() <= off).all(), ((buf.loss.double() - want).abs() / off).max()
+    assert B.mlmc_get_status(ctx) == B.MLMC_OK
+
+
 # ------------------------------------------------------------------------------------------ refusals
 def test_tensors_on_another_gpu_than_the_context(B, ctx):
     assert ctx.device == 0
