@@ -658,10 +658,14 @@ constexpr int kTopSmemMost = 200 * 1024;
 template <typename T, int THREADS>
 void launch_threads(Workspace& ws, TopPlan& p, cudaStream_t s) {
     // As many blocks per row, a power of two, as are resident at a time for all rows, while each has a batch per thread (64 x 131,072 fp32,
-    // 256 threads: 20 us with one, 14 with four, 17 with six, 16 with eight).  Sections of at most 2^17 logits unless k is large: a section
-    // may send k entries, and all together have to fit.
+    // 256 threads: 20 us with one, 14 with four, 17 with six, 16 with eight).  A section may send k entries, and all together have to fit.
+    // Rows of 1 MB and more whose k is large have sections of 2^17 logits at most, whatever their number: the second look at k groups of
+    // several trips is long (700 x 262,144 fp32, k = 256: 192 us so, 228 with a block per row; 160 x 2^20 bf16, k = 500: 116 and 150).  For
+    // others it is not worth a cluster's barriers (700 x 300,000 bf16, k = 700: 262 us with two blocks, 187 with one; 400 x 262,144 fp32,
+    // k = 128: 107 and 91; 2048 x 160,000 bf16, k = 100: 169 and 149; but 300 x 2^20 fp32, k = 20: 233 with eight, 243 with one).
     int most = 1;
     while (most < kRowClusterMost && 2 * most * p.k <= 2048) most *= 2;
+    const bool large = p.V * (int64_t)sizeof(T) >= 1 << 20 && p.k >= 256;
     size_t smem;
     int blocks = most;
     for (;; blocks /= 2) {
@@ -675,7 +679,7 @@ void launch_threads(Workspace& ws, TopPlan& p, cudaStream_t s) {
         p.groups = ((trips + (1 << p.log_span) - 1) >> p.log_span) + 2;
         smem = top_smem<THREADS>(p.groups, p.room, blocks > 1);
         const int per_sm = std::min<int>(kResident<true, THREADS> / THREADS, (int)(227 * 1024 / (smem + sizeof(TopShared<THREADS>) + 1024)));
-        if (blocks == 1 || p.V > (int64_t)(blocks / 2) << 17) break;
+        if (blocks == 1 || (large && p.V > (int64_t)(blocks / 2) << 17)) break;
         if (p.N * blocks <= (int64_t)per_sm * ws.sm_count && p.V > (int64_t)(blocks / 2) * THREADS * kBatch<T>) break;
     }
     const unsigned grid = (unsigned)(p.N * blocks);

@@ -140,7 +140,7 @@ def test_continuations_of_two_beams_next_to_one_another(B, ctx, V, scale, T):
 
 # ------------------------------------------------------------------------------------------ the rest, wherever it lies
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("N, V, k", [(3, 1 << 20, 1024), (3, 1 << 20, 512), (4, 262_147, 700), (40, 131_075, 128), (330, 131_075, 128),
+@pytest.mark.parametrize("N, V, k", [(3, 1 << 20, 1024), (3, 1 << 20, 512), (4, 262_147, 700), (40, 131_075, 128), (330, 131_075, 128), (330, 262_147, 128),
                                      (300, 40_000, 300), (20, 9001, 1000), (500, 3001, 60), (330, 1244, 64), (300, 398, 99)])
 def test_a_rest_of_a_few_logits(B, ctx, N, V, k, dtype):
     """All but the message and n <= 12 logits of 0 is -inf, or so low that it does not count: one of them that is lost, or taken twice, changes
@@ -166,6 +166,14 @@ def test_a_rest_of_a_few_logits(B, ctx, N, V, k, dtype):
         assert torch.equal(out.idx.long().sort(1).values, sent.sort(1).values)
         want = n.double().log() - z.max(1).values.double()
         assert ((out.rest.double() - want).abs() <= (12 + 4 * 4) * U + 2 * U * want.abs()).all()
+    assert B.mlmc_get_status(ctx) == B.MLMC_OK
+
+
+@pytest.mark.parametrize("N, V, k, dtype", [(400, 150_001, 50, torch.float32), (310, 262_147, 128, torch.float32), (300, 262_147, 256, torch.float32),
+                                            (600, 160_001, 512, torch.bfloat16), (297, 1 << 20, 20, torch.bfloat16), (100, 1 << 20, 500, torch.bfloat16)])
+def test_top_logits_of_many_very_long_rows(B, ctx, N, V, k, dtype):
+    """A block per row, of groups of up to 16 trips, or sections of it."""
+    check_top(B, ctx, rows_of(V, N, dtype, V + k), k, 1.0)
     assert B.mlmc_get_status(ctx) == B.MLMC_OK
 
 
