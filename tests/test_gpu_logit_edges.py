@@ -294,6 +294,48 @@ def test_small_losses_keep_their_digits_at_high_temperatures(B, ctx, N, V, k, T,
     assert B.mlmc_get_status(ctx) == B.MLMC_OK
 
 
+# ------------------------------------------------------------------------------------------ states that grow
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("W", [1, 4, 5])
+def test_states_that_grow_by_a_token(B, ctx, W, in_place):
+    """One table of states for a whole search: heads first, tokens first, a size of one, a part of a larger buffer."""
+    Bn, room = 3, 19
+    n = Bn * W
+    g = torch.Generator(device="cuda").manual_seed(W)
+
+    def caches():
+        def fill(shape, dtype):
+            return torch.randint(-100, 100, shape, generator=g, device="cuda").to(dtype)
+        return [fill((n, 3, room, 24), torch.bfloat16), fill((n, 1, room, 7), torch.float32), fill((n, 5, room, 1), torch.uint8),
+                fill((2, n, 3, room, 8), torch.bfloat16)[1], fill((n, 6, room, 16), torch.float32)[:, 2:4], fill((n, 2, room + 4, 3), torch.bfloat16)[:, :, 2:2 + room]]
+    src = caches()
+    dst = src if in_place else caches()
+    states = B.BeamStates(src if in_place else list(zip(src, dst)), W, tokens=2)
+    text = torch.randint(0, 1000, (n, room), generator=g, device="cuda")
+    lines = B.BeamStates([text], W, tokens=1)
+    for length in (1, 2, 3, 8, 9, room, 5, 0):
+        parent = torch.randint(0, W, (Bn, W), generator=g, device="cuda").int()
+        at = (torch.arange(Bn, device="cuda")[:, None] * W + parent).reshape(-1).long()
+        want = [d.clone() for d in dst]
+        for x, y in zip(src, want):
+            y[:, :, :length] = x[at][:, :, :length]
+        want_text = torch.cat([text[at][:, :length], text[:, length:]], 1)
+        B.mlmc_beam_reorder(ctx, parent, states.first(length))
+        B.mlmc_beam_reorder(ctx, parent, lines.first(length))
+        assert all(torch.equal(x, y) for x, y in zip(dst, want)) and torch.equal(text, want_text)
+    assert B.mlmc_get_status(ctx) == B.MLMC_OK
+
+
+def test_tokens_that_cannot_be_moved(B, ctx):
+    x = torch.zeros((4, 2, 10, 8), device="cuda")
+    states = B.BeamStates([x, torch.zeros((4, 3, 12, 8), device="cuda")], 2, tokens=2)
+    for bad in (lambda: states.first(-1), lambda: states.first(11), lambda: B.BeamStates([x], 2).first(1), lambda: B.BeamStates([x], 2, tokens=0),
+                lambda: B.BeamStates([x], 2, tokens=4), lambda: B.BeamStates([x[:, :, ::2]], 2, tokens=2), lambda: B.BeamStates([x.transpose(2, 3)], 2, tokens=2),
+                lambda: B.BeamStates([x[..., :4]], 2, tokens=2)):
+        with pytest.raises(ValueError):
+            bad()
+
+
 # ------------------------------------------------------------------------------------------ refusals
 def test_tensors_on_another_gpu_than_the_context(B, ctx):
     assert ctx.device == 0
