@@ -157,7 +157,7 @@ def _keep(s):
         s.rows = B.LogitBuffers(case["B"] * case["W"], min(case["K"], V))
         s.out = B.BeamBuffers(case["B"], case["K"])
     elif kind == "reorder":
-        s.states = B.BeamStates([(a[:, :, :case["length"]], b[:, :, :case["length"]]) for a, b in zip(s.src, s.dst)], case["W"])
+        s.states = B.BeamStates(list(zip(s.src, s.dst)), case["W"], tokens=2)  # of the whole caches; how far they are filled is the call's
     else:
         s.rows = B.LogitBuffers.of(s.msg["idx"], s.msg["val"], s.msg["count"], s.msg["rest"])
         s.out = B.DistillBuffers(N)
@@ -188,7 +188,7 @@ def run(s):
             B.mlmc_top_logits(_ctx, s.logits, s.done, T, s.rows)
             B.mlmc_beam_select(_ctx, s.rows, V=case["V"], W=case["W"], T=T, score=s.score, done=s.done, eos=EOS, out=s.out)
             return {"token": s.out.token, "parent": s.out.parent, "score": s.out.score, "done": s.out.done}
-        B.mlmc_beam_reorder(_ctx, s.parent, s.states)
+        B.mlmc_beam_reorder(_ctx, s.parent, s.states.first(case["length"]))
         return s.dst
     if kind == "top":
         return _top(s.logits, case["k"], T)
