@@ -483,12 +483,46 @@ class BeamBuffers:
         self.ref, self.ref_endless = C.byref(self.struct), C.byref(self.endless)
 
 
+_MOST_PIECES = 1 << 22
+
+
+def _meet(entries, beams: int) -> bool:
+    """Whether a state's destination shares bytes with another state (of views between one another up to _MOST_PIECES pieces are looked at)."""
+    spans = []
+    for e in entries:
+        length = (beams - 1) * e.beam_stride + (e.chunks - 1) * e.chunk_stride + e.chunk_bytes
+        spans.append((e.dst, length, True, e))
+        if e.src != e.dst:
+            spans.append((e.src, length, False, e))
+    spans.sort(key=lambda x: x[0])
+    written = anything = -1          # ends of what came before
+    for first, length, dst, _ in spans:
+        if first < (anything if dst else written):
+            break
+        anything = max(anything, first + length)
+        if dst:
+            written = max(written, first + length)
+    else:
+        return False
+    if sum(beams * e.chunks for _, _, _, e in spans) > _MOST_PIECES:
+        return False
+    starts = [(first + np.arange(beams, dtype=np.int64)[:, None] * e.beam_stride + np.arange(e.chunks, dtype=np.int64) * e.chunk_stride).ravel()
+              for first, _, _, e in spans]
+    first = np.concatenate(starts)
+    end = first + np.repeat([e.chunk_bytes for _, _, _, e in spans], [len(x) for x in starts])
+    dst = np.repeat([d for _, _, d, _ in spans], [len(x) for x in starts])
+    order = np.argsort(first, kind="stable")
+    first, end, dst = first[order], end[order], dst[order]
+    anything, written = np.maximum.accumulate(end), np.maximum.accumulate(np.where(dst, end, -1))
+    return bool((first[1:] < np.where(dst[1:], anything[:-1], written[:-1])).any())
+
+
 class BeamStates:
     """States of B * W beams: (source, destination) tensors [B * W, ...], or one tensor that is reordered in place.
 
     Behind the first dimension a state may be strided in one place (a cache [B * W, heads, room, size] cut to the tokens so far);
-    source and destination have the same shape and strides.  The tensors are kept; their shapes and memory are looked up here and not
-    again, which takes some 15 us of the host for each.  For caches that grow, `tokens` is the dimension along which they do (2 above):
+    source and destination have the same shape and strides, and no destination shares memory with another state.  The tensors are kept; their shapes and memory are looked up here and not
+    again, which takes some 10 us of the host for each.  For caches that grow, `tokens` is the dimension along which they do (2 above):
     `first(n)` makes the next call move the first n tokens of it."""
 
     def __init__(self, states, W: int, tokens: Optional[int] = None):
@@ -533,6 +567,8 @@ class BeamStates:
             self.kept.append((src, dst))
         if self.device is None:
             raise ValueError("there are no states")
+        if _meet(entries, self.beams):
+            raise ValueError("the destination of a state shares memory with another state")
         self.n = len(entries)
         self.array = (mlmc_beam_state * max(1, self.n))(*entries)
         self.token_bytes = np.array(token_bytes, dtype=np.int64)

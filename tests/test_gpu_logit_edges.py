@@ -336,6 +336,24 @@ def test_tokens_that_cannot_be_moved(B, ctx):
             bad()
 
 
+def test_states_that_share_memory(B, ctx):
+    """A cache of keys and values side by side is two states; a swap, and one state twice, would race."""
+    n, g = 6, torch.Generator(device="cuda").manual_seed(1)
+    both = torch.randn((n, 4, 2, 9, 8), generator=g, device="cuda")
+    parent = torch.tensor([[2, 0, 0], [1, 1, 2]], dtype=torch.int32, device="cuda")
+    at = torch.tensor([2, 0, 0, 4, 4, 5], device="cuda")
+    want = both.clone()
+    want[:, :, :, :5] = both[at][:, :, :, :5]
+    B.mlmc_beam_reorder(ctx, parent, B.BeamStates([both[:, :, 0], both[:, :, 1]], 3, tokens=2).first(5))
+    assert torch.equal(both, want)
+    x, y = torch.zeros((n, 8), device="cuda"), torch.zeros((n, 8), device="cuda")
+    for bad in ([(x, y), (y, x)], [x, x], [(x, y), x], [(x, y), (torch.ones_like(x), y)]):
+        with pytest.raises(ValueError, match="memory"):
+            B.BeamStates(bad, 3)
+    B.BeamStates([(x, y), (x, torch.zeros_like(x))], 3)
+    assert B.mlmc_get_status(ctx) == B.MLMC_OK
+
+
 # ------------------------------------------------------------------------------------------ refusals
 def test_tensors_on_another_gpu_than_the_context(B, ctx):
     assert ctx.device == 0

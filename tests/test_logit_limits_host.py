@@ -29,3 +29,32 @@ def test_tensors_on_another_gpu_than_the_context():
     for at in ("cuda:0", "cuda:2"):
         with pytest.raises(ValueError):
             B._stream_of(here, torch.device(at))
+
+
+@pytest.mark.parametrize("states, meet", [
+    ([(P, 2 * P, 64, 1, 0, 64), (3 * P, 4 * P, 64, 1, 0, 64)], False),
+    ([(P, P, 64, 1, 0, 64), (2 * P, 2 * P, 64, 1, 0, 64)], False),
+    ([(P, 2 * P, 64, 1, 0, 64), (2 * P, P, 64, 1, 0, 64)], True),                       # a swap
+    ([(P, P, 64, 1, 0, 64), (P, P, 64, 1, 0, 64)], True),                               # one state twice
+    ([(P, 2 * P, 64, 1, 0, 64), (3 * P, 2 * P + 255, 64, 1, 0, 64)], True),             # 4 beams: the last byte
+    ([(P, 2 * P, 64, 1, 0, 64), (3 * P, 2 * P + 256, 64, 1, 0, 64)], False),
+    ([(P, 2 * P, 64, 1, 0, 64), (P, 3 * P, 64, 1, 0, 64)], False),                      # one source, two copies
+    ([(P, 2 * P, 64, 1, 0, 64), (P + 32, 3 * P, 64, 1, 0, 64)], False),
+    ([(P, P, 64, 1, 0, 64), (P + 192, 3 * P, 64, 1, 0, 64)], True),                     # read where another one writes
+    ([(P, P, 256, 1, 0, 128), (P + 128, P + 128, 256, 1, 0, 128)], False),              # between one another: keys and values of a beam
+    ([(P, P, 256, 1, 0, 128), (P + 127, P + 127, 256, 1, 0, 128)], True),
+    ([(P, P, 512, 4, 64, 32), (P + 32, P + 32, 512, 4, 64, 32)], False),                # and of a head
+    ([(P, P, 512, 4, 64, 33), (P + 32, P + 32, 512, 4, 64, 32)], True),
+    ([(P, P, 512, 4, 64, 32), (P + 32, P + 32, 512, 2, 128, 32)], False),               # other strides
+    ([(P, P, 512, 4, 64, 32), (P + 160, P + 160, 512, 2, 32, 32)], True)])              # its second piece
+def test_states_that_meet(states, meet):
+    for order in (states, states[::-1]):
+        assert B._meet([B.mlmc_beam_state(*x) for x in order], 4) is meet
+
+
+def test_states_that_meet_are_looked_for_in_many(monkeypatch):
+    many = [B.mlmc_beam_state(P + 4096 * i, 64 * P + 4096 * i, 1024, 1, 0, 1024) for i in range(300)]
+    assert not B._meet(many, 4)
+    assert B._meet(many + [B.mlmc_beam_state(2 * P, 64 * P + 4096 * 150 + 4095, 1024, 1, 0, 1)], 4)
+    monkeypatch.setattr(B, "_MOST_PIECES", 4)             # views between one another in more pieces than that are taken as they are
+    assert not B._meet([B.mlmc_beam_state(P, P, 64, 1, 0, 64), B.mlmc_beam_state(P, P, 64, 1, 0, 64)], 4)
