@@ -8,11 +8,11 @@
 // writes the gradient gives every entry that, and the entries of S are written over it after a barrier.  Between the two passes there is
 // nothing but the row's sums: rows lie in L2 for the second, or in shared memory.
 //
-// What bounds it: loss of 1000 x 131,072 fp32 89 us, 5.9 TB/s (0.90 of a copy's rate), of 4096 x 32,000 bf16 52 us, 5.0 TB/s: 7 instructions
+// What bounds it (calls): loss of 1000 x 131,072 fp32 96 us, 5.5 TB/s (0.85 of a copy's rate), of 4096 x 32,000 bf16 59 us, 4.4 TB/s: 7 instructions
 // for 32 logits, issue 54 % busy, and a row's beginning and end (message, sums, loss) around 64 KB.  Loss and gradient of 2048 x 131,072 bf16
-// 247 us, 4.4 TB/s: half of the second reads miss L2; of 1000 x 131,072 fp32 206 us, 5.1 TB/s: clusters wait for all of a row before they
-// write any of it.  The gradient by
-// itself, 4096 x 32,000 bf16: 94 us, 5.6 TB/s.  16 rows 4.9 us: a chain of dependent loads (count, index, logit), barriers, the loss.
+// 253 us, 4.3 TB/s: half of the second reads miss L2; of 1000 x 131,072 fp32 217 us, 4.8 TB/s: clusters wait for all of a row before they
+// write any of it.  The gradient by itself, 4096 x 32,000 bf16: 88 us, 6.0 TB/s.  16 rows 6 us, 4.9 of them on the GPU: a chain of
+// dependent loads (count, index, logit), barriers, the loss.  (Choices below compare GPU times in replayed graphs, up to a tenth below a call's.)
 #include <algorithm>
 
 #include "logits.cuh"

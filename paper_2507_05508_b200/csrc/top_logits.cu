@@ -9,10 +9,11 @@
 // Few long rows are cut into sections, the blocks of a cluster: they agree on a floor, and the first block ranks all candidates.
 //
 // What bounds it: the pass runs at what the blocks have in flight, and a quarter of a block's time (floor, list, second look, ranking) asks
-// for nothing.  4096 x 65,536 bf16 102 us, 5.3 TB/s (0.81 of a copy's rate); 1024 x 131,072 fp32 114 us, 4.7 TB/s: the groups' numbers take 35
-// KB of shared memory per row, which leaves four rows per SM; 999 x 50,257 bf16 30 us, 3.4 TB/s: all rows run at once, so what follows
-// their passes overlaps with nothing; one row 8.2 us: 1.4 in the pass, the rest a chain of two cluster and five block barriers.
-// Clusters of two blocks for 999 and 1024 rows: 40 and 140 us.
+// for nothing.  Calls: 4096 x 65,536 bf16 117 us, 4.6 TB/s (0.71 of a copy's rate); 1024 x 131,072 fp32 125 us, 4.3 TB/s: the groups' numbers take
+// 35 KB of shared memory per row, which leaves four rows per SM; 999 x 50,257 bf16 31 us, 3.3 TB/s: all rows run at once, so what follows
+// their passes overlaps with nothing; one row 8.4 us: 1.4 in the pass, the rest a chain of two cluster and five block barriers.
+// (Choices below compare GPU times in replayed graphs, which are up to a tenth below a call's.)  Clusters of two blocks for 999 and 1024
+// rows: 40 and 140 us.
 #include <algorithm>
 
 #include "logits.cuh"
